@@ -420,9 +420,10 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
           }
           const float mine_v = key < Ltot ? raw[TW_KEYS + i] : 0.f, mine_k = raw[i];
           const bool bad = key < Ltot && !(fabsf(mine_v) + fabsf(mine_k) < INFINITY);
-          // Where some row does not see some key, no scale may turn its weight of 0 into a NaN: the rows that do see one that is not
-          // finite are marked instead.
-          if (part == 0) sc[i] = plain || (key < Ltot && !bad) ? mine_k : 1.f;
+          // Where some row does not see some key, that key's scales may be anything (a slot that was never written has zeros), but neither may
+          // make a NaN of a score of -inf or of a weight of 0: the key's is positive and finite (the rows that see a key whose scale is zero
+          // get its scores, zeros, from the smallest one), a value's finite, and the rows that do see a key with others are marked.
+          if (part == 0) sc[i] = plain || (key < Ltot && !bad && mine_k > 0.f) ? mine_k : 1.17549435e-38f;
           else sc[TW_KEYS + i] = plain || !bad ? mine_v * vinv : 0.f;
           if (!plain) {
             const unsigned m = __ballot_sync(0xffffffffu, bad);

@@ -1,0 +1,96 @@
+"""atf_decode_tree: slots that a row does not see, keys that no row sees and slots that were never written do not change the row,
+whatever they hold, in the kernels for up to 8, up to 16 and more rows a KV head."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_02947_b200 as atf
+import step_reference as ref
+
+pytestmark = pytest.mark.gpu
+FORMATS = ["bf16", "e4m3", "int8"]
+ROWS = [1, 2, 3, 16]  # heads of a KV head: 8, 16, 24 and 128 rows beside the 8 nodes below
+PARENTS = [-1, 0, 1, -1, -1, 4, 5, 2]
+NOBODYS = 3           # a node that no other node follows
+HKV, D, T, L, CAP, REACH = 2, 128, 8, 300, 400, 100
+
+
+def _rows(shape, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+
+
+def _inputs(G):
+    return _rows((1, HKV, CAP, D), 1), _rows((1, HKV, CAP, D), 2), _rows((1, HKV * G, T, D), 3)
+
+
+def _attend(c, Q, W, return_lse=True):
+    out = atf.atf_decode_tree(Q, c, L, torch.tensor(PARENTS, dtype=torch.int32, device="cuda"), table=W, return_lse=return_lse)
+    atf.binding.check_status()
+    return out
+
+
+def _check(fmt, Q, K, V, W, O, LSE, nodes, parents=PARENTS, length=L):
+    """Rows of these nodes against the definition on what the cache holds of K, V.
+
+    Tolerances as in test_gpu_tree.py, but for what f16 weights lose below 2^-14: half a step of 2^-24, in units in which the row's
+    largest weight times its value's scale, so far, is at least 2 (kept at 2^7, against a reference that is at most 2^6 too high): 2^-26 of
+    that largest product a key, times a code of at most 448 (or 127), where 448 times a scale is less than 2 max|v| of the row
+    of values (127 times a scale: (1 + 2^-7) max|v|).  2^-25 of the largest p max|v| among the keys that the row sees, a key."""
+    k, v = (ref.held(t[0, :, :length + len(parents)].double().cpu().numpy(), fmt) for t in (K, V))
+    k, v = k[0] * k[1][..., None], v[0] * v[1][..., None]
+    G, h = Q.shape[1] // HKV, D // 2
+    depth, line = ref.tree(parents)
+    place = np.concatenate((np.arange(length), length + depth))
+    q = Q[0].double().cpu().numpy()
+    o, lse = O[0].double().cpu().numpy(), LSE[0].double().cpu().numpy()
+    W = np.asarray(W)
+    for i in nodes:
+        z = length + depth[i] - place
+        seen = np.concatenate((np.ones(length, dtype=bool), line[i])) & (z <= W.max())
+        ks, z = seen.nonzero()[0], z[seen]
+        live = z[:, None] <= W
+        live = np.concatenate((live, live), -1)
+        for hq in range(HKV * G):
+            kk, vv, qq = k[hq // G, ks] * live, v[hq // G, ks], q[hq, i]
+            s = kk @ qq / np.sqrt(D)
+            m = s.max()
+            p = np.exp(s - m)
+            rl = m + np.log(p.sum())
+            p /= p.sum()
+            A = (np.abs(kk) @ np.abs(qq)).max() / np.sqrt(D)
+            w, u = 2.0 ** -18 * A + 2.0 ** -20, (len(ks) / 8 + 64) * 2.0 ** -24
+            assert abs(lse[hq, i] - rl) <= w + u + 2.0 ** -20 * abs(rl), (i, hq, lse[hq, i], rl)
+            tol = (2.0 ** (-8 if fmt == "bf16" else -11) + 2 * w + 2 * u) * (p @ np.abs(vv)) + 2.0 ** -8 * np.abs(p @ vv) * 1.001
+            if fmt != "bf16":
+                tol = tol + len(ks) * 2.0 ** -25 * (p * np.abs(vv).max(-1)).max()
+            off = np.abs(o[hq, i] - p @ vv)
+            assert (off <= tol).all(), (i, hq, (off / tol).max())
+
+
+def _written(fmt, K, V, fill):
+    """A cache whose slots hold K and V where a row but NOBODYS sees them, and elsewhere what `fill` leaves."""
+    c = atf.new_kvcache(1, HKV, CAP, D, fmt)
+    fill(c)
+    near = torch.arange(L - REACH, L + T, device="cuda")
+    near = near[near != L + NOBODYS]
+    atf.atf_kvcache_write(c, K[:, :, near].contiguous(), V[:, :, near].contiguous(), slots=near[None])
+    return c
+
+
+def _scales(value):
+    def fill(c):
+        if c.scales is not None:
+            c.scales.fill_(value)
+    return fill
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G", ROWS)
+@pytest.mark.parametrize("scale", [0.0, -1.0, -float("inf"), float("inf"), float("nan"), 2.0 ** -140])
+def test_slots_that_were_never_written(fmt, G, scale):
+    """A fresh cache holds zeros, scales among them; one made of other memory holds anything."""
+    K, V, Q = _inputs(G)
+    W = torch.tensor([REACH] * (D // 2))
+    O, LSE = _attend(_written(fmt, K, V, _scales(scale)), Q, W)
+    _check(fmt, Q, K, V, W.tolist(), O, LSE, [i for i in range(T) if i != NOBODYS])
