@@ -409,7 +409,7 @@ atf_status atf_kvcache_read(const atf_kvcache* cache, void* K, void* V, int B, i
  *   parents: dev int32, sequence b's at parents + b * parents_step (0: one tree for all, else at least T), or NULL: a chain.
  *   counts: dev int32 [B], nodes of each sequence (taken as 0..T), or NULL: T.  Rows of O and lse behind them stay as they are,
  *   slots behind them are not looked at.
- *   A row is not touched by what it does not see, infinities and NaN among it; a row that sees a key or value that is not finite
+ *   A row is not touched by what it does not see, infinities and NaN and the bytes of slots that were never written among it; a row that sees a key or value that is not finite
  *   comes out NaN.
  *   T <= 128, any Hq / Hkv.  table as in atf_prefill (host, NULL = full attention).
  *   scratch: dev, 256-byte aligned, atf_decode_tree_scratch_bytes(...) bytes (0: not supported), for this call alone: calls that

@@ -378,6 +378,19 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
             pb[k][nb][hf] = tr_movmatrix(F16 ? pack_f16x2(p[0], p[1]) : pack_bf16x2(p[0], p[1]));
           }
 
+      if (FMT == ATF_KV_E4M3 && !FAST && !plain) {  // where the codes stand: in the loop below it would cost the form without masks registers
+        bool found = false;
+#pragma unroll 1
+        for (int o = lane * 16; o < SB * D; o += 512) {
+          uint4* at = const_cast<uint4*>(reinterpret_cast<const uint4*>(vs + kin0 * D + o));
+          const uint4 w = *at, x = make_uint4(without_nan<FMT>(w.x), without_nan<FMT>(w.y), without_nan<FMT>(w.z), without_nan<FMT>(w.w));
+          if (w.x == x.x && w.y == x.y && w.z == x.z && w.w == x.w) continue;
+          *at = x;
+          found = true;
+        }
+        if (found) fence_proxy_async_smem();  // the next tile is copied over them
+        __syncwarp();
+      }
       // ---- O^T += V^T P^T ----
       const bool whole = FAST || kb0 + SB <= Ltot;  // slots behind the last node may hold anything
 #pragma unroll

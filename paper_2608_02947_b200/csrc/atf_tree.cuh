@@ -97,6 +97,14 @@ __device__ __forceinline__ void codes4_f16(uint32_t w, uint32_t& a, uint32_t& b)
     b = *reinterpret_cast<const uint32_t*>(&q);
   }
 }
+// Four codes with zeros in the place of NaN ones.  No row that is written has those, but a slot that was not may, and a key that some row
+// does not see has weight 0 there, which a NaN would not survive.
+template <int FMT>
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+  if (FMT != ATF_KV_E4M3) return w;
+  const uint32_t nan = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes 0x7f and 0xff
+  return w & ~((nan >> 7) * 0xffu);
+}
 // Two codes (the low 16 bits).
 template <int FMT>
 __device__ __forceinline__ uint32_t codes_f16(uint32_t two) {

@@ -481,14 +481,14 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
               w[q][2] = c4.z;
               w[q][3] = c4.w;
             }
-            if (!plain) {  // slots behind the last node may hold anything, a NaN among it
+            if (!plain) {  // slots behind the last node, or that some row does not see, may hold anything, a NaN among it
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 uint32_t m = 0u;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) m |= k0 + kb * 16 + v_key(q, e) < Ltot ? 0xffu << (8 * e) : 0u;
 #pragma unroll
-                for (int d4 = 0; d4 < 4; ++d4) w[q][d4] &= m;
+                for (int d4 = 0; d4 < 4; ++d4) w[q][d4] = without_nan<FMT>(w[q][d4] & m);
               }
             }
 #pragma unroll

@@ -94,3 +94,21 @@ def test_slots_that_were_never_written(fmt, G, scale):
     W = torch.tensor([REACH] * (D // 2))
     O, LSE = _attend(_written(fmt, K, V, _scales(scale)), Q, W)
     _check(fmt, Q, K, V, W.tolist(), O, LSE, [i for i in range(T) if i != NOBODYS])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G", ROWS)
+@pytest.mark.parametrize("byte", [0x7f, 0xff, 0x80])
+def test_bytes_of_slots_that_were_never_written(fmt, G, byte):
+    """0x7f and 0xff are the NaN of e4m3, which no row that is written gets, and of a bf16 bytewise."""
+    K, V, Q = _inputs(G)
+    W = torch.tensor([REACH] * (D // 2))
+
+    def fill(c):
+        for t in (c.k, c.v) + (() if c.scales is None else (c.scales,)):
+            t.view(torch.uint8).fill_(byte)
+        if c.scales is not None:
+            c.scales[..., ::2] = 1.0
+
+    O, LSE = _attend(_written(fmt, K, V, fill), Q, W)
+    _check(fmt, Q, K, V, W.tolist(), O, LSE, [i for i in range(T) if i != NOBODYS])
