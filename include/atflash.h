@@ -411,6 +411,10 @@ atf_status atf_kvcache_read(const atf_kvcache* cache, void* K, void* V, int B, i
  *   slots behind them are not looked at.
  *   A row is not touched by what it does not see, infinities and NaN and the bytes of slots that were never written among it; a row that sees a key or value that is not finite
  *   comes out NaN.
+ *   8-bit: a weight times its value's scale is rounded to 16 bits, relative to the largest such product among the keys that the row sees:
+ *   to 2^-11 of itself, below 2^-20 of the largest to 2^-31 of that.  (Both within a factor of 2^6, by which scales of keys that are
+ *   taken together are not told apart.)  The scales of a sequence's values lie within 2^100 of one another, rows of zeros apart: a
+ *   row that sees a value which lies further above the first ones comes out NaN.
  *   T <= 128, any Hq / Hkv.  table as in atf_prefill (host, NULL = full attention).
  *   scratch: dev, 256-byte aligned, atf_decode_tree_scratch_bytes(...) bytes (0: not supported), for this call alone: calls that
  *   overlap on the GPU, two captured graphs among them, need one each.  Its contents need not be set.  A workspace has to be

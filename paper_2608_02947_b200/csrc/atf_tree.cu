@@ -110,7 +110,8 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
     m_used[nb][0] = m_used[nb][1] = -INFINITY;
     l_part[nb][0] = l_part[nb][1] = 0.f;
   }
-  float vref = 0.f;  // 8-bit: what the sums' values are measured in, the largest value scale so far
+  // 8-bit: unit of the values' scales (zero until one is met), by what they are multiplied, and up to where they are taken as they stand
+  float vunit = 0.f, vinv = 0.f, vtop = 0.f;
 
   if (warp == TR_WARPS) {
     // =============================== producer ===============================
@@ -276,6 +277,55 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
           }
       }
 
+      // ---- 8-bit: scales of the values ----
+      float v2[NK][2], lv[NK][2];  // in the unit, and log2 of that
+      if (F16) {
+        bool larger = false;
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const int i = k * 16 + hf * 8 + g;
+            v2[k][hf] = FAST || kb0 + i < Ltot ? vscale[kin0 + i] : 0.f;
+            larger |= v2[k][hf] > vtop;
+          }
+        if (__any_sync(0xffffffffu, larger)) {  // than before: rows of zeros, whose scale is 1, do not count
+          float x = 0.f, least = 3e38f;
+#pragma unroll
+          for (int k = 0; k < NK; ++k) {
+            const uint32_t zero = zero_rows<D, FMT>(vs + (kin0 / 16 + k) * (16 * D), lane);
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              float& v = v2[k][hf];
+              if (v < 3e38f && (zero >> (hf * 8 + g) & 1u) != 0u) v = 0.f;
+              x = fmaxf(x, v < 3e38f ? v : 0.f);
+              least = fminf(least, v > 0.f ? v : 3e38f);
+            }
+          }
+          x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
+          least = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(least)));
+          if (vunit == 0.f) {
+            const float2 u = value_unit(x);
+            vunit = u.x;
+            vinv = u.y;
+          }
+          // up to 64 times as large is taken as it stands from now on; a few large ones, that no row may see, are looked at again
+          if (x <= least * TR_V_EVEN) vtop = fmaxf(vtop, fminf(x * TR_V_EVEN, vunit * TR_V_MOST));
+#pragma unroll
+          for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+              if (v2[k][hf] * vinv > TR_V_MOST) v2[k][hf] = __uint_as_float(0x7fc00000u);
+        }
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            v2[k][hf] *= vinv;
+            lv[k][hf] = value_log2(v2[k][hf]);
+          }
+      }
+
       // ---- scaling, mask, online softmax (log2 domain) ----
       float mx[NB][2];
 #pragma unroll
@@ -303,7 +353,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
                 }
                 s = seen ? s : -INFINITY;
               }
-              mx[nb][e] = fmaxf(mx[nb][e], s);
+              mx[nb][e] = fmaxf(mx[nb][e], F16 ? s + lv[k][hf] : s);
             }
         }
       bool moved = false;
@@ -324,31 +374,6 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
           }
           bias[nb][e] = (F16 ? TR_P_SHIFT : 0.f) - (m == -INFINITY ? 0.f : m);
         }
-      // 8-bit: the values' reference grows with the largest scale (a NaN row does not move it)
-      float vfix = 1.f, v2[NK][2];
-      if (F16) {
-        float x = 0.f;
-#pragma unroll
-        for (int k = 0; k < NK; ++k)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const int i = k * 16 + hf * 8 + g;
-            v2[k][hf] = FAST || kb0 + i < Ltot ? vscale[kin0 + i] : 0.f;
-            x = fmaxf(x, v2[k][hf] < 3e38f ? v2[k][hf] : 0.f);
-          }
-        x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
-        if (x > vref) {
-          vfix = vref / x;
-          vref = x;
-          moved = true;
-        }
-        const float vinv = vref > 0.f ? __fdividef(1.f, vref) : 0.f;
-#pragma unroll
-        for (int k = 0; k < NK; ++k) {
-          v2[k][0] *= vinv;
-          v2[k][1] *= vinv;
-        }
-      }
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -357,7 +382,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
 #pragma unroll
           for (int mt = 0; mt < NMT; ++mt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) oacc[nb][mt][e] *= fix[nb][e & 1] * vfix;
+            for (int e = 0; e < 4; ++e) oacc[nb][mt][e] *= fix[nb][e & 1];
         }
       }
       uint32_t pb[NK][NB][2];  // B fragments: keys 2 t4 + {0, 1} (+ 8) of row g
@@ -499,8 +524,8 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
         if (F16) {
 #pragma unroll
           for (int J = 0; J < D / 32; ++J)
-            *reinterpret_cast<float4*>(dst + 32 * J + 4 * g) = make_float4(oacc[nb][2 * J][e] * vref, oacc[nb][2 * J][2 + e] * vref,
-                                                                           oacc[nb][2 * J + 1][e] * vref, oacc[nb][2 * J + 1][2 + e] * vref);
+            *reinterpret_cast<float4*>(dst + 32 * J + 4 * g) = make_float4(oacc[nb][2 * J][e] * vunit, oacc[nb][2 * J][2 + e] * vunit,
+                                                                           oacc[nb][2 * J + 1][e] * vunit, oacc[nb][2 * J + 1][2 + e] * vunit);
         } else {
 #pragma unroll
           for (int mt = 0; mt < NMT; ++mt) {

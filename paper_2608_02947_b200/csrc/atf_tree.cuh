@@ -7,7 +7,11 @@
 
 constexpr int TR_MAX_NODES = 128;
 constexpr float TR_RESCALE = 7.f;  // log2 units by which a row's maximum may outgrow its reference before sums are rescaled
-constexpr float TR_P_SHIFT = 7.f;  // 8-bit: weights are kept times 2^7, so that 2^-21 of a row's largest is still a full f16
+// 8-bit: f16 holds a weight times its value's scale, 2^7 times as large, against a reference of the row: the largest such product among the keys
+// that the row sees, so far.  2^-21 of it is still a full f16, and nothing that a row does not see moves its reference.
+constexpr float TR_P_SHIFT = 7.f;
+constexpr float TR_V_EVEN = 64.f;          // scales of a block of keys within this factor are not told apart where that saves work
+constexpr float TR_V_MOST = 1.2676506e30f;  // 2^100: how far scales may lie from the first one that was met (weights and sums are fp32)
 
 struct TreeParams {
   const __nv_bfloat16* q;  // [B, Hq, T, D]
@@ -104,6 +108,32 @@ __device__ __forceinline__ uint32_t without_nan(uint32_t w) {
   if (FMT != ATF_KV_E4M3) return w;
   const uint32_t nan = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes 0x7f and 0xff
   return w & ~((nan >> 7) * 0xffu);
+}
+// Scales of values are taken relative to a power of two near the first one that is met: the unit, and by what to multiply.
+__device__ __forceinline__ float2 value_unit(float scale) {
+  const uint32_t bits = min(__float_as_uint(scale), 253u << 23) & 0x7f800000u;  // up to 2^126, whose inverse is normal
+  return bits == 0u ? make_float2(0.f, 0.f) : make_float2(__uint_as_float(bits), __uint_as_float((254u << 23) - bits));
+}
+// log2 of a value's relative scale, for references; what is smaller than 2^-100, zeros among it, counts as that.
+__device__ __forceinline__ float value_log2(float v) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(v, 1.f / TR_V_MOST)));
+  return y;
+}
+// The keys of a 16-key block of V whose codes are all zero, one bit a key.  Rows of zeros have scale 1, whatever the size of the others.
+template <int D, int FMT>
+__device__ __forceinline__ uint32_t zero_rows(const uint8_t* block, int lane) {
+  const int t = lane >> 3;
+  uint32_t any = 0u, keys = 0u;
+#pragma unroll 1
+  for (int c = lane & 7; c < D / 4; c += 8) {
+    const uint4 w = *reinterpret_cast<const uint4*>(block + v_chunk<D>(t, c));
+    any |= w.x | w.y | w.z | w.w;
+  }
+  if (FMT == ATF_KV_E4M3) any &= 0x7f7f7f7fu;  // a zero may have a sign
+#pragma unroll
+  for (int e = 0; e < 4; ++e) keys |= (any >> (8 * e) & 0xffu) != 0u ? 1u << v_key(t, e) : 0u;
+  return ~__reduce_or_sync(0xffffffffu, keys) & 0xffffu;
 }
 // Two codes (the low 16 bits).
 template <int FMT>

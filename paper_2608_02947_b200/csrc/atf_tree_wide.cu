@@ -127,7 +127,8 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
   __shared__ unsigned long long s_bad[ST][2];  // keys of a step (stage of V in bf16, of K in 8 bits) that make a row which sees them NaN
   __shared__ int s_groups[ST];              // groups of 8 pairs that the scores of a stage of K contract
   __shared__ int s_lone[ST];                // the step has terms that only some rows keep
-  __shared__ float2 s_vref[2];              // 8-bit, of even / odd steps: what the values' weights are measured in, and the change to it
+  __shared__ float s_vtop[2];               // 8-bit, of even / odd steps: log2 of the largest scale of a value; -inf where they differ much
+  __shared__ float s_vunit;                 // what the scales are measured in
   __shared__ uint32_t s_tmem;
   __shared__ int s_near, s_far, s_abort;
   const uint32_t sbase = (smem_u32(dsm_raw) + 1023u) & ~1023u;
@@ -327,7 +328,7 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
       // =============================== operands ===============================
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TW_REGS_PREP));
       const int pt = threadIdx.x - TW_PREP * 32, i = pt & 63, part = pt >> 6;  // two threads a key
-      float vref = 0.f, vinv = 1.f;
+      float vunit = 0.f, vinv = 0.f, vtop = 0.f;  // see atf_tree_tiles
       for (int t = 0; t < mine; ++t) {
         const int st = t % ST, k0 = (s_first + t * P.nsplit) * TW_KEYS, key = k0 + i;
         const uint32_t kr = sK + st * S::KSTAGE, vr = sV + st * S::VSTAGE;
@@ -402,23 +403,47 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
             *reinterpret_cast<uint4*>(kop + j * (TW_KEYS * 32) + sw) = make_uint4(w[0], w[1], w[2], w[3]);
             *reinterpret_cast<uint4*>(kop + j * (TW_KEYS * 32) + (16 ^ sw)) = make_uint4(w[4], w[5], w[6], w[7]);
           }
-          // scales of the keys; weights of the values: their scale over the largest one so far (a row that is not finite is left out of that)
+          // scales of the keys; weights of the values: their scale in the unit (one that is not finite sets nothing)
           float* sc = reinterpret_cast<float*>(sgen + S::SC_OFF) + (t & 1) * (2 * TW_KEYS);
           const float* raw = reinterpret_cast<const float*>(sgen + S::K_OFF + st * S::KSTAGE + S::KBYTES);
-          float x = 0.f;
+          float x = 0.f, v[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float v = k0 + lane + 32 * e < Ltot ? raw[TW_KEYS + lane + 32 * e] : 0.f;
-            x = fmaxf(x, v < 3e38f ? v : 0.f);
+            v[e] = k0 + lane + 32 * e < Ltot ? raw[TW_KEYS + lane + 32 * e] : 0.f;
+            x = fmaxf(x, v[e] < 3e38f ? v[e] : 0.f);
           }
           x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
-          float fix = 1.f;
-          if (x > vref) {
-            fix = vref / x;
-            vref = x;
-            vinv = 1.f / x;
+          const float mine_k = raw[i], even = x * (1.f / TR_V_EVEN);
+          float mine_v = key < Ltot ? raw[TW_KEYS + i] : 0.f;
+          bool uneven = false;
+          if (__builtin_expect(__any_sync(0xffffffffu, even > vtop || (v[0] > 0.f && v[0] < even) || (v[1] > 0.f && v[1] < even)), 0)) {
+            // They differ from before or from each other: rows of zeros, whose scale is 1, do not count.
+            if (!warp_wait(bar(VFULL, st), (t / ST) & 1)) { fail_site = 75; break; }
+            float least = 3e38f;
+            x = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              uint32_t zero = 0u;
+#pragma unroll 1
+              for (int kb = 0; kb < 32; kb += 16) zero |= zero_rows<D, FMT>(sgen + S::V_OFF + st * S::VSTAGE + (32 * e + kb) * D, lane) << kb;
+              const bool none = v[e] > 0.f && v[e] < 3e38f && (zero >> lane & 1u) != 0u;  // behind the last slot, what was there before
+              uneven |= none;
+              if (none) v[e] = 0.f;
+              if (e == (i >> 5)) mine_v = v[e];  // lane = i & 31
+              x = fmaxf(x, v[e] < 3e38f ? v[e] : 0.f);
+              least = fminf(least, v[e] > 0.f ? v[e] : 3e38f);
+            }
+            x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
+            least = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(least)));
+            if (vunit == 0.f) {
+              const float2 u = value_unit(x);
+              vunit = u.x;
+              vinv = u.y;
+            }
+            uneven = __any_sync(0xffffffffu, uneven) || x > least * TR_V_EVEN;
+            if (!uneven) vtop = fmaxf(vtop, fminf(x, vunit * (TR_V_MOST / TR_V_EVEN)));  // a few large ones, that no row may see, are looked at again
+            if (mine_v * vinv > TR_V_MOST) mine_v = __uint_as_float(0x7fc00000u);
           }
-          const float mine_v = key < Ltot ? raw[TW_KEYS + i] : 0.f, mine_k = raw[i];
           const bool bad = key < Ltot && !(fabsf(mine_v) + fabsf(mine_k) < INFINITY);
           // Where some row does not see some key, that key's scales may be anything (a slot that was never written has zeros), but neither may
           // make a NaN of a score of -inf or of a weight of 0: the key's is positive and finite (the rows that see a key whose scale is zero
@@ -430,7 +455,10 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
             if (lane == 0) reinterpret_cast<volatile uint32_t*>(&s_bad[st][part])[warp & 1] = m;
           }
           hand_over(st);  // the softmax warps have left step t - 2: the V part of step t - 1 has waited for its product
-          if (pt == 0) s_vref[t & 1] = make_float2(vref, fix);
+          if (pt == 0) {
+            s_vtop[t & 1] = uneven ? -INFINITY : value_log2(x * vinv);
+            s_vunit = vunit;
+          }
         }
         if (pt == 0) s_groups[st] = ngl;
         fence_proxy_async_smem();
@@ -613,11 +641,25 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
           tc_wait_st();
         }
 
+        // 8-bit, scales of the values that differ much: the reference needs the row's own largest weight times scale.  (Elsewhere the largest
+        // score and the largest scale bound it well enough: an addition and a maximum a cell less.)
+        float top = -INFINITY;
+        if (F16 && __builtin_expect(s_vtop[bf] == -INFINITY, 0)) {
+          const float* sc = reinterpret_cast<const float*>(sgen + S::SC_OFF) + bf * (2 * TW_KEYS);
+#pragma unroll 1
+          for (int c = 0; c < TW_KEYS; c += 8) {
+            float x[8];
+            tc_ld8(tS + c, x);
+            tc_wait_ld_pin(x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i] * sc[c + i] * rs + value_log2(sc[TW_KEYS + c + i]));
+          }
+        }
+
         float2 s[32];
         tc_ld32(tS, reinterpret_cast<uint32_t*>(s));
         tc_ld32(tS + 32, reinterpret_cast<uint32_t*>(s) + 32);
         const float4* sck = reinterpret_cast<const float4*>(sgen + S::SC_OFF) + bf * (2 * TW_KEYS / 4);  // scales of the keys, then weights of the values
-        const float vfix = F16 ? s_vref[bf].y : 1.f;
         tc_wait_ld_pin64(reinterpret_cast<float(&)[64]>(s));
         if (F16) {
 #pragma unroll
@@ -633,9 +675,9 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
           mx0 = max3(mx0, s[c].x, s[c].y);
           mx1 = max3(mx1, s[c + 1].x, s[c + 1].y);
         }
-        const float mx = fmaxf(mx0, mx1) * rs;
+        const float mx = F16 ? fmaxf(fmaf(fmaxf(mx0, mx1), rs, s_vtop[bf]), top) : fmaxf(mx0, mx1) * rs;
         float fix = 1.f;
-        bool moved = F16 && vfix != 1.f;
+        bool moved = false;
         if (mx > m_used + (m_used == -INFINITY ? 0.f : TR_RESCALE)) {
           fix = m_used == -INFINITY ? 0.f : tr_ex2(m_used - mx);
           m_used = mx;
@@ -648,7 +690,6 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
           if (t > 0) {
             if (!warp_wait(odone((t - 1) & 1), ((t - 1) >> 1) & 1)) { fail_site = 77; ok = false; break; }
             tc_fence_after();
-            fix *= vfix;
 #pragma unroll 1
             for (int c = 0; c < D; c += 8) {
               float o[8];
@@ -689,11 +730,11 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
       if (ok && mine > 0 && !warp_wait(odone((mine - 1) & 1), ((mine - 1) >> 1) & 1)) { fail_site = 78; ok = false; }
       tc_fence_after();
       if (ok) {
-        const float l = l2.x + l2.y, vref = F16 ? (mine > 0 ? s_vref[(mine - 1) & 1].x : 0.f) : 1.f;
+        const float l = l2.x + l2.y, vunit = F16 ? (mine > 0 ? s_vunit : 0.f) : 1.f;
         const int row = row0 + rr;
         const int64_t o = ((int64_t)b * P.Hq + hkv * G + row % G) * T + row / G, at = (grp * P.nsplit + split) * (int64_t)(T * G) + row;
         const bool direct = P.nsplit == 1;
-        const float f = direct ? (l > 0.f || l != l ? vref / l : 0.f) : vref;
+        const float f = direct ? (l > 0.f || l != l ? vunit / l : 0.f) : vunit;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           float x[32];  // dims c .. c + 31

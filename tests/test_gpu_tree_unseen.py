@@ -87,7 +87,7 @@ def _scales(value):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("G", ROWS)
-@pytest.mark.parametrize("scale", [0.0, -1.0, -float("inf"), float("inf"), float("nan"), 2.0 ** -140])
+@pytest.mark.parametrize("scale", [0.0, -1.0, -float("inf"), float("inf"), float("nan"), 2.0 ** 126, 2.0 ** -140])
 def test_slots_that_were_never_written(fmt, G, scale):
     """A fresh cache holds zeros, scales among them; one made of other memory holds anything."""
     K, V, Q = _inputs(G)
@@ -98,7 +98,7 @@ def test_slots_that_were_never_written(fmt, G, scale):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("G", ROWS)
-@pytest.mark.parametrize("byte", [0x7f, 0xff, 0x80])
+@pytest.mark.parametrize("byte", [0x7f, 0xff, 0x80, 0x55])
 def test_bytes_of_slots_that_were_never_written(fmt, G, byte):
     """0x7f and 0xff are the NaN of e4m3, which no row that is written gets, and of a bf16 bytewise."""
     K, V, Q = _inputs(G)
@@ -112,3 +112,76 @@ def test_bytes_of_slots_that_were_never_written(fmt, G, byte):
 
     O, LSE = _attend(_written(fmt, K, V, fill), Q, W)
     _check(fmt, Q, K, V, W.tolist(), O, LSE, [i for i in range(T) if i != NOBODYS])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G", ROWS)
+@pytest.mark.parametrize("power", [20, 40, 90, -90])
+def test_finite_rows_of_other_sizes(fmt, G, power):
+    """Values of 2^power and more in a node and in keys out of the window (or, the other way, only there of ordinary size): finite,
+    and not seen."""
+    K, V, Q = _inputs(G)
+    W = torch.tensor([REACH] * (D // 2))
+    far = torch.arange(CAP, device="cuda") < L - REACH
+    far[L + NOBODYS] = True
+    V = torch.where(far[:, None], (V.double() * 2.0 ** max(power, 0)), V.double() * 2.0 ** min(power, 0)).to(torch.bfloat16)
+    c = atf.new_kvcache(1, HKV, CAP, D, fmt)
+    atf.atf_kvcache_write(c, K, V)
+    O, LSE = _attend(c, Q, W)
+    _check(fmt, Q, K, V, W.tolist(), O, LSE, range(T))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G", ROWS)
+@pytest.mark.parametrize("first", [True, False])
+def test_large_values_of_no_weight(fmt, G, first):
+    """Keys that every row sees, whose values are 2^40 times as large and whose weights are e^-70 and less; where they come first the
+    other keys are met after them."""
+    K, V, Q = _inputs(G)
+    Q = Q.abs()
+    at = torch.arange(CAP, device="cuda")
+    low = (at < 60) if first else (at >= 200) & (at < L) & (at % 3 == 0)
+    K = torch.where(low[:, None], torch.full_like(K, -12.0), K * 0.25)
+    V = torch.where(low[:, None], (V.double() * 2.0 ** 40).to(torch.bfloat16), V)
+    c = atf.new_kvcache(1, HKV, CAP, D, fmt)
+    atf.atf_kvcache_write(c, K, V)
+    O, LSE = _attend(c, Q, None)
+    _check(fmt, Q, K, V, [CAP] * (D // 2), O, LSE, range(T))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G", ROWS)
+@pytest.mark.parametrize("power", [-30, -60, -100])
+@pytest.mark.parametrize("zeros", ["one", "first", "most"])
+def test_rows_of_zeros_among_small_values(fmt, G, power, zeros):
+    """A row of zeros has scale 1, whatever the size of its neighbours."""
+    K, V, Q = _inputs(G)
+    at = torch.arange(CAP, device="cuda")
+    none = {"one": at == 150, "first": at < 140, "most": at % 9 != 4}[zeros]
+    V = torch.where(none[:, None], torch.zeros_like(V), (V.double() * 2.0 ** power).to(torch.bfloat16))
+    c = atf.new_kvcache(1, HKV, CAP, D, fmt)
+    atf.atf_kvcache_write(c, K, V)
+    O, LSE = _attend(c, Q, None)
+    _check(fmt, Q, K, V, [CAP] * (D // 2), O, LSE, range(T))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G,nodes", [(1, 5), (2, 8), (3, 64)])
+def test_sizes_that_change_along_the_text(fmt, G, nodes):
+    """Values that grow and shrink by 2^80 along a long text, in steps and from row to row, over several splits."""
+    length = 9000
+    K, V, Q = _rows((1, HKV, length + nodes, D), 1), _rows((1, HKV, length + nodes, D), 2), _rows((1, HKV * G, nodes, D), 3)
+    at = torch.arange(length + nodes, device="cuda", dtype=torch.float64)
+    par = [i // 2 - 1 for i in range(nodes)]
+    pt = torch.tensor(par, dtype=torch.int32, device="cuda")
+    for power in (40 * torch.sin(at / 700), torch.floor(at / 1500) * 13 - 40, -torch.floor(at / 1500) * 13 + 40,
+                  40 - 80 * torch.rand(at.shape, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda", dtype=torch.float64)):
+        Vp = (V.double() * torch.exp2(power)[:, None]).to(torch.bfloat16)
+        Kp = K.double().clone()
+        Kp[..., 7] -= power * 2  # the larger the values, the smaller the weights where q[7] is positive, and the other way round
+        Kp = Kp.to(torch.bfloat16)
+        c = atf.new_kvcache(1, HKV, length + nodes, D, fmt)
+        atf.atf_kvcache_write(c, Kp, Vp)
+        O, LSE = atf.atf_decode_tree(Q, c, length, pt, return_lse=True)
+        atf.binding.check_status()
+        _check(fmt, Q, Kp, Vp, [length + nodes] * (D // 2), O, LSE, range(0, nodes, 7), par, length)
