@@ -137,6 +137,9 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
         }
       }
     }
+    // no copy is in flight when the sums go where the ring was and the block ends, whatever the others gave up
+    for (int i = max(0, it - ST); i < it; ++i)
+      if (!mbar_wait(full_bar(i % ST), (i / ST) & 1)) fail_site = 62;
   } else {
     // =============================== consumers ===============================
     // word ((row / 8) NKS + j) 32 + lane, register: pair 8 j + 2 t + c of row g is register c of lane 4 g + t
