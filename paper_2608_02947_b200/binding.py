@@ -651,10 +651,17 @@ def _cache_tensor(t, name, dtype):
 
 class KVCache:
     """A key/value cache of `capacity` slots per (batch, KV head): format "bf16" (the group-major K cache of
-    new_kcache_groups and V rows), "e4m3" or "int8" (codes and a scale a row; layouts in include/atflash.h)."""
+    new_kcache_groups and V rows), "e4m3" or "int8" (codes and a scale a row; layouts in include/atflash.h).
+    Its tensors are checked, and their addresses taken, once: an object stands for these tensors and its attributes do not change
+    (their contents do).  For other tensors make another object."""
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name} of a KVCache does not change: make another KVCache")
+
+    __delattr__ = lambda self, name: self.__setattr__(name, None)  # noqa: E731
 
     def __init__(self, fmt, k, v, scales, capacity):
-        self.format = f = _KV_FORMATS.get(fmt)
+        f = _KV_FORMATS.get(fmt)
         if f is None:
             raise AtfError(2, f"cache format must be one of {sorted(_KV_FORMATS)}")
         bf16 = f == ATF_KV_BF16
@@ -674,13 +681,20 @@ class KVCache:
             raise AtfError(1, "the cache's v does not match its k")
         if not bf16 and scales.shape != (B, Hkv, tiles, 2, kt):
             raise AtfError(1, "the cache's scales must be [B,Hkv,tiles,2,KT]")
-        self.index = index = k.get_device()
+        index = k.get_device()
         if v.get_device() != index or (not bf16 and scales.get_device() != index):
             raise AtfError(1, "the cache's tensors must be on the same CUDA device")
-        self.k, self.v, self.scales, self.capacity = k, v, None if bf16 else scales, capacity
-        self.B, self.Hkv, self.d, self.device = B, Hkv, d, k.device
-        self._c = _KVCache(f, k.data_ptr(), v.data_ptr(), None if bf16 else scales.data_ptr(), capacity)
-        self._ref = C.byref(self._c)
+        c = _KVCache(f, k.data_ptr(), v.data_ptr(), None if bf16 else scales.data_ptr(), capacity)
+        self.__dict__.update(format=f, k=k, v=v, scales=None if bf16 else scales, capacity=capacity, B=B, Hkv=Hkv, d=d, index=index,
+                             device=k.device, _c=c, _ref=C.byref(c))
+
+
+def _cache_ref(cache):
+    """The cache as the library takes it.  Memory that was taken from under its tensors (set_, .data) is not written to."""
+    c = cache._c
+    if cache.k.data_ptr() != c.k or cache.v.data_ptr() != c.v or (c.scales is not None and cache.scales.data_ptr() != c.scales):
+        raise AtfError(1, "the cache's tensors have other memory than when the KVCache was made")
+    return cache._ref
 
 
 @functools.lru_cache(maxsize=16)
@@ -713,7 +727,7 @@ def atf_kvcache_write(cache, K, V, pos0=0, slots=None):
     sp = _dev_ints(slots, "slots", torch.int64, (cache.B, n))
     index = cache.index
     with _on(index, K, V, slots):
-        code = lib().atf_kvcache_write(cache._ref, K.data_ptr(), sk, V.data_ptr(), sv, cache.B, cache.Hkv, n, d, pos0, sp,
+        code = lib().atf_kvcache_write(_cache_ref(cache), K.data_ptr(), sk, V.data_ptr(), sv, cache.B, cache.Hkv, n, d, pos0, sp,
                                        torch._C._cuda_getCurrentRawStream(index))
     if code:
         _check(code)
@@ -728,7 +742,7 @@ def atf_kvcache_read(cache, n, pos0=0, slots=None, K=None, V=None):
     K, V = _out(K, "K", shape, torch.bfloat16, cache.k), _out(V, "V", shape, torch.bfloat16, cache.k)
     index = cache.index
     with _on(index, K, V, slots):
-        code = lib().atf_kvcache_read(cache._ref, K.data_ptr(), V.data_ptr(), cache.B, cache.Hkv, shape[2], cache.d, pos0, sp,
+        code = lib().atf_kvcache_read(_cache_ref(cache), K.data_ptr(), V.data_ptr(), cache.B, cache.Hkv, shape[2], cache.d, pos0, sp,
                                       torch._C._cuda_getCurrentRawStream(index))
     if code:
         _check(code)
@@ -785,7 +799,7 @@ def atf_decode_tree(Q, cache, lens, parents=None, table=None, counts=None, max_l
     if _ws is None or _ws.get_device() != index:
         ensure_workspace(atf_workspace_bytes(ATF_OP_DECODE, 1, 1, 1, 1, 64), cache.device)
     with _on(index, Q, lens, parents, counts, O, LSE):
-        code = lib().atf_decode_tree(Q.data_ptr(), cache._ref, lp, max_len, pp, pstep, cp, O.data_ptr(), lsep, B, Hq, cache.Hkv, T, d, tab,
+        code = lib().atf_decode_tree(Q.data_ptr(), _cache_ref(cache), lp, max_len, pp, pstep, cp, O.data_ptr(), lsep, B, Hq, cache.Hkv, T, d, tab,
                                      scratch.data_ptr(), scratch.numel(), torch._C._cuda_getCurrentRawStream(index))
     if code:
         _check(code)
