@@ -292,21 +292,35 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
             v2[k][hf] = FAST || kb0 + i < Ltot ? vscale[kin0 + i] : 0.f;
             larger |= v2[k][hf] > vtop;
           }
-        if (__any_sync(0xffffffffu, larger)) {  // than before: rows of zeros, whose scale is 1, do not count
-          float x = 0.f, least = 3e38f;
+        if (__any_sync(0xffffffffu, larger)) {  // than before
+          float x, least;
+          bool one;
+          auto range = [&]() {
+            x = 0.f;
+            least = 3e38f;
+            one = false;
 #pragma unroll
-          for (int k = 0; k < NK; ++k) {
-            const uint32_t zero = zero_rows<D, FMT>(vs + (kin0 / 16 + k) * (16 * D), lane);
+            for (int k = 0; k < NK; ++k)
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              float& v = v2[k][hf];
-              if (v < 3e38f && (zero >> (hf * 8 + g) & 1u) != 0u) v = 0.f;
-              x = fmaxf(x, v < 3e38f ? v : 0.f);
-              least = fminf(least, v > 0.f ? v : 3e38f);
-            }
+              for (int hf = 0; hf < 2; ++hf) {
+                const float v = v2[k][hf];
+                x = fmaxf(x, v < 3e38f ? v : 0.f);
+                least = fminf(least, v > 0.f ? v : 3e38f);
+                one |= v == 1.f;
+              }
+            x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
+            least = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(least)));
+          };
+          range();
+          if (__any_sync(0xffffffffu, one) || x > least * TR_V_EVEN) {  // rows of zeros, whose scale is 1 whatever the others are, do not count
+            const uint32_t zero = zero_rows<D, FMT>(vs + kin0 * D, lane);
+#pragma unroll
+            for (int k = 0; k < NK; ++k)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf)
+                if (v2[k][hf] < 3e38f && (zero >> (k * 16 + hf * 8 + g) & 1u) != 0u) v2[k][hf] = 0.f;
+            range();
           }
-          x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
-          least = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(least)));
           if (vunit == 0.f) {
             const float2 u = value_unit(x);
             vunit = u.x;

@@ -120,20 +120,24 @@ __device__ __forceinline__ float value_log2(float v) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(v, 1.f / TR_V_MOST)));
   return y;
 }
-// The keys of a 16-key block of V whose codes are all zero, one bit a key.  Rows of zeros have scale 1, whatever the size of the others.
+// The keys of two 16-key blocks of V whose codes are all zero, one bit a key.  Rows of zeros have scale 1, whatever the size of the others.
 template <int D, int FMT>
-__device__ __forceinline__ uint32_t zero_rows(const uint8_t* block, int lane) {
+__device__ __forceinline__ uint32_t zero_rows(const uint8_t* blocks, int lane) {
   const int t = lane >> 3;
-  uint32_t any = 0u, keys = 0u;
+  uint32_t keys = 0u;
 #pragma unroll 1
-  for (int c = lane & 7; c < D / 4; c += 8) {
-    const uint4 w = *reinterpret_cast<const uint4*>(block + v_chunk<D>(t, c));
-    any |= w.x | w.y | w.z | w.w;
-  }
-  if (FMT == ATF_KV_E4M3) any &= 0x7f7f7f7fu;  // a zero may have a sign
+  for (int kb = 0; kb < 32; kb += 16) {
+    uint32_t any = 0u;
+#pragma unroll 1
+    for (int c = lane & 7; c < D / 4; c += 8) {
+      const uint4 w = *reinterpret_cast<const uint4*>(blocks + kb * D + v_chunk<D>(t, c));
+      any |= w.x | w.y | w.z | w.w;
+    }
+    if (FMT == ATF_KV_E4M3) any &= 0x7f7f7f7fu;  // a zero may have a sign
 #pragma unroll
-  for (int e = 0; e < 4; ++e) keys |= (any >> (8 * e) & 0xffu) != 0u ? 1u << v_key(t, e) : 0u;
-  return ~__reduce_or_sync(0xffffffffu, keys) & 0xffffu;
+    for (int e = 0; e < 4; ++e) keys |= (any >> (8 * e) & 0xffu) != 0u ? 1u << (kb + v_key(t, e)) : 0u;
+  }
+  return ~__reduce_or_sync(0xffffffffu, keys);
 }
 // Two codes (the low 16 bits).
 template <int FMT>

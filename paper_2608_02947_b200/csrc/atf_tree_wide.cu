@@ -96,6 +96,21 @@ __device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
 
+// 8-bit, rare: the largest weight times scale of this thread's row (log2), cell by cell.  A function of its own: its code in the loop of the
+// softmax costs the steps that do not need it (32 nodes of 131072, e4m3: 132 us, with it in the loop 136).
+__device__ __noinline__ float row_top(uint32_t tS, const float* sc, float rs) {
+  float top = -INFINITY;
+#pragma unroll 1
+  for (int c = 0; c < TW_KEYS; c += 8) {
+    float x[8];
+    tc_ld8(tS + c, x);
+    tc_wait_ld_pin(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i] * sc[c + i] * rs + value_log2(sc[TW_KEYS + c + i]));
+  }
+  return top;
+}
+
 // A step of 64 keys: pairs live at its farthest distance, at its nearest key for every row, and there for some row.
 struct StepPairs {
   int far, all, any;
@@ -417,15 +432,13 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
           float mine_v = key < Ltot ? raw[TW_KEYS + i] : 0.f;
           bool uneven = false;
           if (__builtin_expect(__any_sync(0xffffffffu, even > vtop || (v[0] > 0.f && v[0] < even) || (v[1] > 0.f && v[1] < even)), 0)) {
-            // They differ from before or from each other: rows of zeros, whose scale is 1, do not count.
+            // They differ from before or from each other: rows of zeros, whose scale is 1 whatever the others are, do not count.
             if (!warp_wait(bar(VFULL, st), (t / ST) & 1)) { fail_site = 75; break; }
             float least = 3e38f;
             x = 0.f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              uint32_t zero = 0u;
-#pragma unroll 1
-              for (int kb = 0; kb < 32; kb += 16) zero |= zero_rows<D, FMT>(sgen + S::V_OFF + st * S::VSTAGE + (32 * e + kb) * D, lane) << kb;
+              const uint32_t zero = zero_rows<D, FMT>(sgen + S::V_OFF + st * S::VSTAGE + e * (32 * D), lane);
               const bool none = v[e] > 0.f && v[e] < 3e38f && (zero >> lane & 1u) != 0u;  // behind the last slot, what was there before
               uneven |= none;
               if (none) v[e] = 0.f;
@@ -644,17 +657,7 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
         // 8-bit, scales of the values that differ much: the reference needs the row's own largest weight times scale.  (Elsewhere the largest
         // score and the largest scale bound it well enough: an addition and a maximum a cell less.)
         float top = -INFINITY;
-        if (F16 && __builtin_expect(s_vtop[bf] == -INFINITY, 0)) {
-          const float* sc = reinterpret_cast<const float*>(sgen + S::SC_OFF) + bf * (2 * TW_KEYS);
-#pragma unroll 1
-          for (int c = 0; c < TW_KEYS; c += 8) {
-            float x[8];
-            tc_ld8(tS + c, x);
-            tc_wait_ld_pin(x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i] * sc[c + i] * rs + value_log2(sc[TW_KEYS + c + i]));
-          }
-        }
+        if (F16 && __builtin_expect(s_vtop[bf] == -INFINITY, 0)) top = row_top(tS, reinterpret_cast<const float*>(sgen + S::SC_OFF) + bf * (2 * TW_KEYS), rs);
 
         float2 s[32];
         tc_ld32(tS, reinterpret_cast<uint32_t*>(s));
