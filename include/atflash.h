@@ -409,8 +409,10 @@ atf_status atf_kvcache_read(const atf_kvcache* cache, void* K, void* V, int B, i
  *   parents: dev int32, sequence b's at parents + b * parents_step (0: one tree for all, else at least T), or NULL: a chain.
  *   counts: dev int32 [B], nodes of each sequence (taken as 0..T), or NULL: T.  Rows of O and lse behind them stay as they are,
  *   slots behind them are not looked at.
- *   A row is not touched by what it does not see, infinities and NaN and the bytes of slots that were never written among it; a row that sees a key or value that is not finite
- *   comes out NaN.
+ *   A row is not touched by what it does not see, infinities and NaN and the bytes of slots that were never written among it.  A row
+ *   that sees a value which is not finite is NaN, O and lse; so is one that sees an 8-bit row of keys which was not finite.  A bf16 key
+ *   with infinities or NaN has the score that q k gives over the pairs in its reach: a NaN or +inf makes NaN of the row, with -inf the
+ *   key has no weight.  (Finite values whose weighted sum passes the fp32 range make NaN of the row as well.)
  *   8-bit: a weight times its value's scale is rounded to 16 bits, relative to the largest such product among the keys that the row sees:
  *   to 2^-11 of itself, below 2^-20 of the largest to 2^-31 of that.  (Both within a factor of 2^6, by which scales of keys that are
  *   taken together are not told apart.)  The scales of a sequence's values lie within 2^100 of one another, rows of zeros apart: a

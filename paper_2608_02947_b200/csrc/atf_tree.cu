@@ -345,6 +345,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
 
       // ---- scaling, mask, online softmax (log2 domain) ----
       float mx[NB][2];
+      uint32_t hidden = 0u;  // bf16: cells that their rows do not see, which a score of -inf alone does not tell (8-bit keys give none that is not masked)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) mx[nb][0] = mx[nb][1] = -INFINITY;
 #pragma unroll
@@ -369,6 +370,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
                   seen = j < n && ((tr.line[cur][node][(j >> 6) & 1] >> (j & 63)) & 1ull) != 0ull && tr.depth[cur][node] - tr.depth[cur][min(j, n - 1)] <= Wmax;
                 }
                 s = seen ? s : -INFINITY;
+                if (!F16) hidden |= seen ? 0u : 1u << (((k * 2 + hf) * NB + nb) * 2 + e);
               }
               mx[nb][e] = fmaxf(mx[nb][e], F16 ? s + lv[k][hf] : s);
             }
@@ -491,7 +493,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (((odd >> (g + 8 * (e >> 1))) & 1u) != 0u && sc[k][nb][e] != -INFINITY) l_part[nb][e & 1] = __uint_as_float(0x7fc00000u);
+                if (((odd >> (g + 8 * (e >> 1))) & 1u) != 0u && (hidden >> (((k * 2 + (e >> 1)) * NB + nb) * 2 + (e & 1)) & 1u) == 0u) l_part[nb][e & 1] = __uint_as_float(0x7fc00000u);
           }
         }
       }
@@ -553,8 +555,9 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
       }
   }
   __syncthreads();
-  for (int idx = threadIdx.x; idx < rows * (D / 4); idx += TR_THREADS) {  // four dims of a row
-    const int rr = idx / (D / 4), col = idx % (D / 4) * 4, row = row0 + rr;
+  for (int i0 = warp * 32; i0 < rows * (D / 4); i0 += TR_THREADS) {  // four dims of a row a lane, D / 4 lanes a row
+    const bool in = i0 + lane < rows * (D / 4);
+    const int idx = in ? i0 + lane : i0, rr = idx / (D / 4), col = idx % (D / 4) * 4, row = row0 + rr;
     float m[TR_WARPS], M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < TR_WARPS; ++w) {
@@ -576,11 +579,14 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
       lacc = fmaf(f, src[D + 1], lacc);
     }
     if (P.nsplit == 1) {
+      const unsigned odd = __ballot_sync(0xffffffffu, in && not_finite(acc.x, acc.y, acc.z, acc.w));
+      if ((odd & (D == 64 ? 0xffffu << (lane & 16) : 0xffffffffu)) != 0u) lacc = __uint_as_float(0x7fc00000u);
+      if (!in) continue;
       const int64_t o = ((int64_t)b * P.Hq + hkv * G + row % G) * T + row / G;
       const float inv = lacc > 0.f || lacc != lacc ? 1.f / lacc : 0.f;
       *reinterpret_cast<uint2*>(P.O + o * D + col) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
       if (P.lse && col == 0) P.lse[o] = (M + log2f(lacc) - (F16 ? TR_P_SHIFT : 0.f)) * 0.6931471805599453f;
-    } else {
+    } else if (in) {
       const int64_t at = (grp * P.nsplit + split) * (int64_t)(T * G) + row;
       *reinterpret_cast<float4*>(P.outs + at * D + col) = acc;
       if (col == 0) *reinterpret_cast<float2*>(P.sums + at * 2) = make_float2(M, lacc);
@@ -631,6 +637,7 @@ __global__ void __launch_bounds__(TM_THREADS) atf_tree_join(const __grid_constan
       for (int c = 0; c < D / 32; ++c) acc[c] = fmaf(w, x[i][c], acc[c]);
     }
   }
+  if (__any_sync(0xffffffffu, not_finite(acc[0], acc[1], acc[D / 32 - 2], acc[D / 32 - 1]))) L = __uint_as_float(0x7fc00000u);
   const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) P.O[o * D + c * 32 + lane] = __float2bfloat16_rn(acc[c] * inv);

@@ -152,6 +152,13 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Of a row's sums.  A row that has met a value which is not finite is NaN as a whole, its LSE with it: which of its elements an infinity or a
+// NaN gets to depends on the block of keys that it stands in.
+__device__ __forceinline__ bool not_finite(float a, float b, float c, float d) {
+  const float z = fmaf(a, 0.f, b * 0.f) + fmaf(c, 0.f, d * 0.f);
+  return z != z;
+}
+
 // Rows of Q (node, head of the KV head's group) into shared memory: warp `w` of NW takes every NW-th of ROWS rows, U of them in flight;
 // store(row of the block, pair from the lowest frequency, its two dims) gets every word, zeros behind the last row.  A lane has two
 // neighbouring pairs of a row.  8-bit caches: a row is stored as f16, multiplied by the power of two that brings its largest element

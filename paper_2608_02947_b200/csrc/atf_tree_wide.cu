@@ -734,6 +734,7 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
       tc_fence_after();
       if (ok) {
         const float l = l2.x + l2.y, vunit = F16 ? (mine > 0 ? s_vunit : 0.f) : 1.f;
+        bool odd = false;
         const int row = row0 + rr;
         const int64_t o = ((int64_t)b * P.Hq + hkv * G + row % G) * T + row / G, at = (grp * P.nsplit + split) * (int64_t)(T * G) + row;
         const bool direct = P.nsplit == 1;
@@ -760,6 +761,8 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
             for (int k = 0; k < 32; ++k) x[k] = mine > 0 ? x[k] * f : 0.f;
             if (direct) {
 #pragma unroll
+              for (int k = 0; k < 32; k += 4) odd |= not_finite(x[k], x[k + 1], x[k + 2], x[k + 3]);
+#pragma unroll
               for (int k = 0; k < 32; k += 8)
                 *reinterpret_cast<uint4*>(P.O + o * D + c + k) = make_uint4(pack_bf16x2(x[k], x[k + 1]), pack_bf16x2(x[k + 2], x[k + 3]),
                                                                             pack_bf16x2(x[k + 4], x[k + 5]), pack_bf16x2(x[k + 6], x[k + 7]));
@@ -769,9 +772,13 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
             }
           }
         }
+        if (direct && odd) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4*>(P.O + o * D + c) = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+        }
         if (rr < rows) {
           if (!direct) *reinterpret_cast<float2*>(P.sums + at * 2) = make_float2(m_used, l);
-          else if (P.lse) P.lse[o] = (m_used + log2f(l) - (F16 ? TR_P_SHIFT : 0.f)) * 0.6931471805599453f;
+          else if (P.lse) P.lse[o] = odd ? __uint_as_float(0x7fc00000u) : (m_used + log2f(l) - (F16 ? TR_P_SHIFT : 0.f)) * 0.6931471805599453f;
         }
       }
       }
