@@ -6,7 +6,8 @@
 // One read and one write of each row: bound by memory.  d/16 lanes hold a row, each the eight pairs of 16 bytes of either half,
 // so that the sum of squares is a few shuffles and the rotation needs no other lane.  The angle is reduced to a fraction of a
 // turn in 64 bits (positions past 2^20 keep their full accuracy), its sine and cosine, the norm and the rotation are fp32, and
-// the result is rounded once.  A thread evaluates its eight angles once and walks the heads of its token.
+// the result is rounded once.  A thread evaluates its eight angles once and walks the heads of its token.  Where a mean square comes near the ends
+// of the range of 32 bits, the squares are taken again of a row that is shifted by a power of two: a vote a head, else.
 #include <algorithm>
 #include <cmath>
 
@@ -27,7 +28,7 @@ struct NormRopeParams {
   NormRopeSide side[2];  // queries, keys
   const int64_t* positions;  // [B, N], or null
   int64_t N, rows, pos0;     // rows = B N
-  float eps;
+  float eps, eps_up, eps_down;  // as it is, and for rows times 2^100 and times 2^-70
   double turn[ATF_MAX_PAIRS];  // theta / (2 pi)
 };
 
@@ -135,7 +136,21 @@ __global__ void __launch_bounds__(NR_THREADS, U * (int)sizeof(T) > 4 ? 2 : 3) at
         for (int i = 0; i < 8; ++i) ss += f[i] * f[i] + g[i] * g[i];
 #pragma unroll
         for (int off = 1; off < LPR; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-        const float inv = rsqrtf(ss * (1.f / D) + P.eps);
+        const float ms = ss * (1.f / D) + P.eps;
+        float inv = rsqrtf(ms);
+        constexpr uint32_t LEAST = 27u << 23, MOST = 227u << 23;  // 2^-100, 2^100
+        const uint32_t bits = __float_as_uint(ms);
+        if (__builtin_expect(__any_sync(0xffffffffu, bits - LEAST >= MOST - LEAST), 0)) {
+          const bool up = bits < LEAST, down = bits >= MOST;
+          const float by = up ? 1.2676506e30f : down ? 8.4703295e-22f : 1.f;  // 2^100, 2^-70: the squares of whatever is left stay in range
+          float s2 = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s2 += (f[i] * by) * (f[i] * by) + (g[i] * by) * (g[i] * by);
+#pragma unroll
+          for (int off = 1; off < LPR; off <<= 1) s2 += __shfl_xor_sync(0xffffffffu, s2, off);
+          const float again = rsqrtf(s2 * (1.f / D) + (up ? P.eps_up : P.eps_down)) * by;
+          if (up || down) inv = again;
+        }
         float a[8], z[8], w[8], v[8];
         wl.get(w);
         wh.get(v);
@@ -215,6 +230,8 @@ extern "C" atf_status atf_qk_norm_rope(const void* Q, const atf_row_strides* q_s
   P.rows = (int64_t)B * N;
   P.pos0 = pos0;
   P.eps = (float)eps;
+  P.eps_up = (float)std::ldexp(eps, 200);
+  P.eps_down = (float)std::ldexp(eps, -140);
   for (int r = 0; r < ATF_MAX_PAIRS; ++r) {
     if (r < d / 2 && !std::isfinite(theta[r])) return atf_fail(ATF_ERR_INVALID_ARG, "%s: theta[%d] is not finite", who, r);
     P.turn[r] = r < d / 2 ? theta[r] / 6.283185307179586476925 : 0.0;
