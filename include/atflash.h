@@ -358,7 +358,7 @@ enum { ATF_DTYPE_BF16 = 0, ATF_DTYPE_F32 = 1 };
  *   theta: host, d/2 doubles.  positions: dev int64 [B, N], or NULL: row n sits at pos0 + n.
  *   The angle is reduced in fp64; the norm, sine, cosine and rotation are fp32, rounded once to `dtype`.  Rows of any size are
  *   normalised, but for rows of subnormals with eps 0, whose reciprocal passes the fp32 range; with eps 0 a row of zeros is NaN, as its
- *   formula is; a row with an infinity or a NaN is NaN.                                                                            */
+ *   formula is.  A NaN makes NaN of its row; an infinity zeros of all elements but its pair, which is NaN.                         */
 atf_status atf_qk_norm_rope(const void* Q, const atf_row_strides* q_strides, const void* K, const atf_row_strides* k_strides,
                             const void* q_weight, const void* k_weight, double eps, void* Qo, void* Ko, int B, int Hq, int Hkv,
                             int64_t N, int d, int dtype, const double* theta, int64_t pos0, const int64_t* positions, void* stream);
