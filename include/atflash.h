@@ -391,7 +391,11 @@ int64_t atf_kvcache_tile_keys(int format, int d); /* 0 for a format or d that is
  *   [B, n], n <= 1024) row i of sequence b goes to slots[b, i], a row whose slot is negative or not below the capacity is left
  *   out, and of rows with the same slot the last stays.  Other slots keep what they hold.
  * atf_kvcache_read: the way back, into contiguous bf16 K, V [B, Hkv, n, d] (code * scale rounded once); a row whose slot is
- *   out of the cache reads as zeros.  A slot may be read any number of times.                                            */
+ *   out of the cache reads as zeros.  A slot may be read any number of times.
+ *   K and V overlap neither the cache nor one another where they are written.
+ *   Rows that move, read and written again at other slots: bf16 and e4m3 rows keep their values (e4m3 a code's power of two may go over
+ *   to the scale), an int8 row does not: what is read is rounded to bf16 and gets a scale of its own, which is off by up to
+ *   half a code of the new scale and 2^-9 of the value, at every move.  Write accepted int8 rows from the K and V that they came from. */
 atf_status atf_kvcache_write(const atf_kvcache* cache, const void* K, const atf_row_strides* k_strides, const void* V,
                              const atf_row_strides* v_strides, int B, int Hkv, int64_t n, int d, int64_t pos0,
                              const int64_t* slots, void* stream);

@@ -736,7 +736,8 @@ def atf_kvcache_write(cache, K, V, pos0=0, slots=None):
 
 def atf_kvcache_read(cache, n, pos0=0, slots=None, K=None, V=None):
     """Rows pos0..pos0+n-1 of the cache, or the rows in slots [B,n], as bf16 (K, V), each [B,Hkv,n,d].  Given K and V receive
-    them; a row whose slot is out of the cache reads as zeros."""
+    them; a row whose slot is out of the cache reads as zeros.  (int8 rows that are read and written elsewhere lose up to a code each
+    time: write them from where they came from.)"""
     shape = (cache.B, cache.Hkv, int(n), cache.d)
     sp = _dev_ints(slots, "slots", torch.int64, (cache.B, shape[2]))
     K, V = _out(K, "K", shape, torch.bfloat16, cache.k), _out(V, "V", shape, torch.bfloat16, cache.k)
