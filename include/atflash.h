@@ -410,7 +410,8 @@ atf_status atf_kvcache_read(const atf_kvcache* cache, void* K, void* V, int B, i
  *   positions) counts iff z <= table[r], and a key that no pair reaches is dropped.  Exact mode; softmax scale 1/sqrt(d).
  *   Q, O: dev bf16 [B, Hq, T, d], Q rotated at the nodes' positions; lse: dev fp32 [B, Hq, T] or NULL.
  *   lens: dev int32 [B], each taken as at most max_len, or NULL: max_len for every sequence.  max_len + T <= capacity; it bounds
- *   the launch, so that a captured call serves every length up to it.
+ *   the launch, so that a captured call serves every length up to it.  The work is split for it: far above the lengths (a large cache
+ *   with little in it) it costs up to half as much again.
  *   parents: dev int32, sequence b's at parents + b * parents_step (0: one tree for all, else at least T), or NULL: a chain.
  *   counts: dev int32 [B], nodes of each sequence (taken as 0..T), or NULL: T.  Rows of O and lse behind them stay as they are,
  *   slots behind them are not looked at.
@@ -419,9 +420,9 @@ atf_status atf_kvcache_read(const atf_kvcache* cache, void* K, void* V, int B, i
  *   with infinities or NaN has the score that q k gives over the pairs in its reach: a NaN or +inf makes NaN of the row, with -inf the
  *   key has no weight.  (Finite values whose weighted sum passes the fp32 range make NaN of the row as well.)
  *   8-bit: a weight times its value's scale is rounded to 16 bits, relative to the largest such product among the keys that the row sees:
- *   to 2^-11 of itself, below 2^-20 of the largest to 2^-31 of that.  (Both within a factor of 2^6, by which scales of keys that are
- *   taken together are not told apart.)  The scales of a sequence's values lie within 2^100 of one another, rows of zeros apart: a
- *   row that sees a value which lies further above the first ones comes out NaN.
+ *   to 2^-11 of itself, below 2^-21 of the largest to 2^-32 of that.  (Both within a factor of 2^6, by which scales of keys that are
+ *   taken together are not told apart.  A row of zeros has scale 1.)  Sums are fp32: rows whose values are all below 2^-110, or some
+ *   above 2^110, are less exact.
  *   T <= 128, any Hq / Hkv.  table as in atf_prefill (host, NULL = full attention).
  *   scratch: dev, 256-byte aligned, atf_decode_tree_scratch_bytes(...) bytes (0: not supported), for this call alone: calls that
  *   overlap on the GPU, two captured graphs among them, need one each.  Its contents need not be set.  A workspace has to be

@@ -12,7 +12,7 @@
 // quarter of the tile's keys each.  S^T = K Q^T and O^T += V^T P^T are mma.sync products (m16n8k16) with keys or dims as M and 8
 // or 16 rows of the tree as N: bf16 for the bf16 cache, f16 for the 8-bit ones, whose codes f16 holds exactly (Q is shifted into
 // its range row by row, which rounds nothing that 28 bits below the row's largest element keep; a weight times its value's
-// scale is kept below 2^16 by a running reference).  The scale of a key multiplies its row of S^T, in 32 bits.  Weights are rounded
+// scale is kept below 2^16 by a running reference of the row, see TR_P_SHIFT).  The scale of a key multiplies its row of S^T, in 32 bits.  Weights are rounded
 // to the type of V, which the product wants; their sum is that of the unrounded ones, in fp32.
 // More than 16 rows take the kernel of atf_tree_wide.cu.
 #include <algorithm>
@@ -110,8 +110,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
     m_used[nb][0] = m_used[nb][1] = -INFINITY;
     l_part[nb][0] = l_part[nb][1] = 0.f;
   }
-  // 8-bit: unit of the values' scales (zero until one is met), by what they are multiplied, and up to where they are taken as they stand
-  float vunit = 0.f, vinv = 0.f, vtop = 0.f;
+  float vtop = 0.f;  // 8-bit: up to where the values' scales are taken as they stand
 
   if (warp == TR_WARPS) {
     // =============================== producer ===============================
@@ -171,7 +170,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
       for (int e = 0; e < 2; ++e) rs[nb][e] = F16 ? kScale * s_qs[nb * 8 + 2 * t4 + e] : kScale;
     // One block of keys of a warp.  FAST: every row sees every key and keeps the same pairs of a key as the others do, as nearly all blocks
     // of a long context are; the form for the others, with its masks and lone terms, is code of its own that stays out of the way.
-    // (One token, 32 x 8 x 16384, e4m3, with the general form wherever a window ends within a block: 177 us instead of 141.)
+    // (One token, 32 x 8 x 16384, e4m3, with the general form wherever a window ends within a block: 135 us instead of 115.)
     auto step = [&](auto form, const uint8_t* ks, int t, int kin0, int kb0, bool committed, bool plain, int n_far, int n_all, int n_any) __attribute__((always_inline)) {
       constexpr bool FAST = decltype(form)::value;
       const bool uniform = n_any == n_far;
@@ -281,7 +280,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
       }
 
       // ---- 8-bit: scales of the values ----
-      float v2[NK][2], lv[NK][2];  // in the unit, and log2 of that
+      float v2[NK][2], lv[NK][2];  // and log2 of them
       if (F16) {
         bool larger = false;
 #pragma unroll
@@ -321,26 +320,13 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
                 if (v2[k][hf] < 3e38f && (zero >> (k * 16 + hf * 8 + g) & 1u) != 0u) v2[k][hf] = 0.f;
             range();
           }
-          if (vunit == 0.f) {
-            const float2 u = value_unit(x);
-            vunit = u.x;
-            vinv = u.y;
-          }
           // up to 64 times as large is taken as it stands from now on; a few large ones, that no row may see, are looked at again
-          if (x <= least * TR_V_EVEN) vtop = fmaxf(vtop, fminf(x * TR_V_EVEN, vunit * TR_V_MOST));
-#pragma unroll
-          for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-              if (v2[k][hf] * vinv > TR_V_MOST) v2[k][hf] = __uint_as_float(0x7fc00000u);
+          if (x <= least * TR_V_EVEN) vtop = fmaxf(vtop, x * TR_V_EVEN);
         }
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            v2[k][hf] *= vinv;
-            lv[k][hf] = value_log2(v2[k][hf]);
-          }
+          for (int hf = 0; hf < 2; ++hf) lv[k][hf] = value_log2(v2[k][hf]);
       }
 
       // ---- scaling, mask, online softmax (log2 domain) ----
@@ -387,7 +373,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
           float& m = m_used[nb][e];
           fix[nb][e] = 1.f;
           if (x > m + (m == -INFINITY ? 0.f : TR_RESCALE)) {
-            fix[nb][e] = m == -INFINITY ? 0.f : tr_ex2(m - x);
+            fix[nb][e] = m == -INFINITY ? 0.f : tr_ex2(F16 ? 0.5f * (m - x) : m - x);  // 8-bit: its root, since it may pass the range of a float
             m = x;
             moved = true;
           }
@@ -396,12 +382,15 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          l_part[nb][0] *= fix[nb][0];
-          l_part[nb][1] *= fix[nb][1];
 #pragma unroll
-          for (int mt = 0; mt < NMT; ++mt)
+          for (int again = 0; again < (F16 ? 2 : 1); ++again) {
+            l_part[nb][0] *= fix[nb][0];
+            l_part[nb][1] *= fix[nb][1];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) oacc[nb][mt][e] *= fix[nb][e & 1];
+            for (int mt = 0; mt < NMT; ++mt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[nb][mt][e] *= fix[nb][e & 1];
+          }
         }
       }
       uint32_t pb[NK][NB][2];  // B fragments: keys 2 t4 + {0, 1} (+ 8) of row g
@@ -536,15 +525,17 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
         float* dst = sm + (warp * ROWS + nb * 8 + 2 * t4 + e) * PS;
+        // 8-bit: references lie apart as the scales do; the parts are joined by their weight in the row, and their outputs are averages
+        const float inv = l == 0.f ? 0.f : __fdividef(1.f, l);
         if (g == 0) {
-          dst[D] = m_used[nb][e];
-          dst[D + 1] = l;
+          dst[D] = F16 ? m_used[nb][e] + tr_lg2(l) - TR_P_SHIFT : m_used[nb][e];  // -inf for no weight
+          dst[D + 1] = F16 ? l * inv : l;                                         // 1, 0, or a NaN
         }
         if (F16) {
 #pragma unroll
           for (int J = 0; J < D / 32; ++J)
-            *reinterpret_cast<float4*>(dst + 32 * J + 4 * g) = make_float4(oacc[nb][2 * J][e] * vunit, oacc[nb][2 * J][2 + e] * vunit,
-                                                                           oacc[nb][2 * J + 1][e] * vunit, oacc[nb][2 * J + 1][2 + e] * vunit);
+            *reinterpret_cast<float4*>(dst + 32 * J + 4 * g) = make_float4(oacc[nb][2 * J][e] * inv, oacc[nb][2 * J][2 + e] * inv,
+                                                                           oacc[nb][2 * J + 1][e] * inv, oacc[nb][2 * J + 1][2 + e] * inv);
         } else {
 #pragma unroll
           for (int mt = 0; mt < NMT; ++mt) {
@@ -585,7 +576,7 @@ atf_tree_tiles(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ 
       const int64_t o = ((int64_t)b * P.Hq + hkv * G + row % G) * T + row / G;
       const float inv = lacc > 0.f || lacc != lacc ? 1.f / lacc : 0.f;
       *reinterpret_cast<uint2*>(P.O + o * D + col) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-      if (P.lse && col == 0) P.lse[o] = (M + log2f(lacc) - (F16 ? TR_P_SHIFT : 0.f)) * 0.6931471805599453f;
+      if (P.lse && col == 0) P.lse[o] = (M + log2f(lacc)) * 0.6931471805599453f;
     } else if (in) {
       const int64_t at = (grp * P.nsplit + split) * (int64_t)(T * G) + row;
       *reinterpret_cast<float4*>(P.outs + at * D + col) = acc;
@@ -641,7 +632,7 @@ __global__ void __launch_bounds__(TM_THREADS) atf_tree_join(const __grid_constan
   const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) P.O[o * D + c * 32 + lane] = __float2bfloat16_rn(acc[c] * inv);
-  if (P.lse && lane == 0) P.lse[o] = (M + log2f(L) - (F16 ? TR_P_SHIFT : 0.f)) * 0.6931471805599453f;
+  if (P.lse && lane == 0) P.lse[o] = (M + log2f(L)) * 0.6931471805599453f;
 }
 
 atf_status launch_join(int format, const TreeParams& P, int B, int d, cudaStream_t s) {

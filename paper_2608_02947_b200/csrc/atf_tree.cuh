@@ -8,10 +8,10 @@
 constexpr int TR_MAX_NODES = 128;
 constexpr float TR_RESCALE = 7.f;  // log2 units by which a row's maximum may outgrow its reference before sums are rescaled
 // 8-bit: f16 holds a weight times its value's scale, 2^7 times as large, against a reference of the row: the largest such product among the keys
-// that the row sees, so far.  2^-21 of it is still a full f16, and nothing that a row does not see moves its reference.
+// that the row sees, so far.  2^-21 of it is still a full f16, and nothing that a row does not see moves its reference.  The row's sum of weights
+// has the same reference: they are fp32 and may be as much smaller or larger than 1 as scales are.
 constexpr float TR_P_SHIFT = 7.f;
-constexpr float TR_V_EVEN = 64.f;          // scales of a block of keys within this factor are not told apart where that saves work
-constexpr float TR_V_MOST = 1.2676506e30f;  // 2^100: how far scales may lie from the first one that was met (weights and sums are fp32)
+constexpr float TR_V_EVEN = 64.f;  // scales of a block of keys within this factor are not told apart where that saves work
 
 struct TreeParams {
   const __nv_bfloat16* q;  // [B, Hq, T, D]
@@ -109,17 +109,14 @@ __device__ __forceinline__ uint32_t without_nan(uint32_t w) {
   const uint32_t nan = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes 0x7f and 0xff
   return w & ~((nan >> 7) * 0xffu);
 }
-// Scales of values are taken relative to a power of two near the first one that is met: the unit, and by what to multiply.
-__device__ __forceinline__ float2 value_unit(float scale) {
-  const uint32_t bits = min(__float_as_uint(scale), 253u << 23) & 0x7f800000u;  // up to 2^126, whose inverse is normal
-  return bits == 0u ? make_float2(0.f, 0.f) : make_float2(__uint_as_float(bits), __uint_as_float((254u << 23) - bits));
-}
-// log2 of a value's relative scale, for references; what is smaller than 2^-100, zeros among it, counts as that.
-__device__ __forceinline__ float value_log2(float v) {
+__device__ __forceinline__ float tr_lg2(float x) {
   float y;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(v, 1.f / TR_V_MOST)));
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// log2 of a value's scale, for references.  What is smaller than 2^-100, zeros among it, counts as that, so that a sum of weights against such a
+// reference stays in the range of fp32.
+__device__ __forceinline__ float value_log2(float scale) { return tr_lg2(fmaxf(scale, 7.8886091e-31f)); }
 // The keys of two 16-key blocks of V whose codes are all zero, one bit a key.  Rows of zeros have scale 1, whatever the size of the others.
 template <int D, int FMT>
 __device__ __forceinline__ uint32_t zero_rows(const uint8_t* blocks, int lane) {
@@ -163,7 +160,7 @@ __device__ __forceinline__ bool not_finite(float a, float b, float c, float d) {
 // store(row of the block, pair from the lowest frequency, its two dims) gets every word, zeros behind the last row.  A lane has two
 // neighbouring pairs of a row.  8-bit caches: a row is stored as f16, multiplied by the power of two that brings its largest element
 // into [2^14, 2^15) (its inverse goes to qs).  U of a block of 128 rows: three; with all twelve of a warp in flight its start is 2000
-// clocks shorter, but what their registers push out is missing in every step (65 / 161 / 130 us with three, 69 / 176 / 139 with twelve).
+// clocks shorter, but what their registers push out is missing in every step (64 / 164 / 133 us with three, 66 / 168 / 140 with twelve).
 template <int D, bool F16, int ROWS, int NW, int U, typename Store>
 __device__ __forceinline__ void stage_rows(const TreeParams& P, int64_t head0, int row0, int rows, int w, int lane, float* qs, Store store) {
   constexpr int H = D / 2;
@@ -216,7 +213,7 @@ __device__ __forceinline__ void stage_rows(const TreeParams& P, int64_t head0, i
 
 // Bounded wait of a thread for a phase of an mbarrier; `abort` (shared by the block) ends the waits of the others once one has given
 // up.  (Tests that may suspend the thread for up to 20 us execute half as many instructions and take longer to answer: 64 x 4 x 32768
-// in bf16 174 us where these took 170.5; 32 x 131072 in e4m3 133.5, 130.)
+// in bf16 165.1 us where these take 164.2; 32 x 131072 in e4m3 138.4, 133.1.)
 __device__ __forceinline__ bool tr_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
   if (mbar_try_wait(bar, parity)) return true;
   const unsigned long long t0 = global_timer_ns();

@@ -12,12 +12,13 @@
 // leaves out of a step's K and V, or convert the codes; 8 copies, 9 issues the scores, 10 the values' products.  The scores of step
 // t + 1 run under step t's softmax; the two blocks of an SM fill each other's waits.
 //
-// What bounds it: no one pipe.  A block's step of 8-bit codes takes about 3100 clocks at two blocks an SM (131072 x 8 heads, 96 rows
-// e4m3: 130 us; memory would take 32, the exponentials 30, the products 25): K's conversion, the scores, the softmax, V's conversion
-// and the product follow one another, and issue slots are 45 % busy.  Blocks of one an SM with steps of 128 keys, with the scores in
-// two or three buffers, with the softmax by halves of the keys or by alternate steps, and K's operands a step ahead were built and
-// measured: 127 to 191 us here, 183 to 222 where this takes 161 (4 x 64 nodes x 32768, bf16), 67 to 77 where it takes 65 (8 x 16
-// nodes x 30011, int8, heads of 64).  mma.sync with 32 rows a block: 1106 / 2300 / 355 us.
+// What bounds it: no one pipe.  131072 x 8 heads, 96 rows, e4m3: 133 us (memory would take 32, the exponentials 30, the products 25).  A block
+// spends 6 us on Q and the tree, 3 until its first scores, 107 (the longest 121) on its 55 steps, 3 on its sums, two blocks an SM; the join
+// is 9.  In a step K's conversion, the scores, the softmax, V's conversion and the product follow one another, and issue slots are 45 % busy.  4 x
+// 64 nodes x 32768 in bf16, nothing to convert: 164 us, 576 blocks in two rounds, each 6, 1, 58 (81) and 3.  Blocks of one an SM with steps of
+// 128 keys, with the scores in two or three buffers, with the softmax by halves of the keys or by alternate steps, and K's operands a step
+// ahead were built and measured: 127 to 191 us where the first took 130, 183 to 222 where the second took 161, 67 to 77 where 8 x 16 nodes x
+// 30011 (int8, heads of 64) took 65.  mma.sync with 32 rows a block: 1106 / 2300 / 355 us.
 //
 // A key's products take the pairs that are live for every row; a (key, pair) term that only some rows keep - where a window ends
 // between the nearest and the farthest row of the tree, a few keys a pair - is added to S in tensor memory by the softmax warps.
@@ -143,7 +144,6 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
   __shared__ int s_groups[ST];              // groups of 8 pairs that the scores of a stage of K contract
   __shared__ int s_lone[ST];                // the step has terms that only some rows keep
   __shared__ float s_vtop[2];               // 8-bit, of even / odd steps: log2 of the largest scale of a value; -inf where they differ much
-  __shared__ float s_vunit;                 // what the scales are measured in
   __shared__ uint32_t s_tmem;
   __shared__ int s_near, s_far, s_abort;
   const uint32_t sbase = (smem_u32(dsm_raw) + 1023u) & ~1023u;
@@ -343,7 +343,7 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
       // =============================== operands ===============================
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TW_REGS_PREP));
       const int pt = threadIdx.x - TW_PREP * 32, i = pt & 63, part = pt >> 6;  // two threads a key
-      float vunit = 0.f, vinv = 0.f, vtop = 0.f;  // see atf_tree_tiles
+      float vtop = 0.f;  // see atf_tree_tiles
       for (int t = 0; t < mine; ++t) {
         const int st = t % ST, k0 = (s_first + t * P.nsplit) * TW_KEYS, key = k0 + i;
         const uint32_t kr = sK + st * S::KSTAGE, vr = sV + st * S::VSTAGE;
@@ -418,7 +418,7 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
             *reinterpret_cast<uint4*>(kop + j * (TW_KEYS * 32) + sw) = make_uint4(w[0], w[1], w[2], w[3]);
             *reinterpret_cast<uint4*>(kop + j * (TW_KEYS * 32) + (16 ^ sw)) = make_uint4(w[4], w[5], w[6], w[7]);
           }
-          // scales of the keys; weights of the values: their scale in the unit (one that is not finite sets nothing)
+          // scales of the keys; scales of the values (one that is not finite counts for nothing)
           float* sc = reinterpret_cast<float*>(sgen + S::SC_OFF) + (t & 1) * (2 * TW_KEYS);
           const float* raw = reinterpret_cast<const float*>(sgen + S::K_OFF + st * S::KSTAGE + S::KBYTES);
           float x = 0.f, v[2];
@@ -448,30 +448,21 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
             }
             x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
             least = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(least)));
-            if (vunit == 0.f) {
-              const float2 u = value_unit(x);
-              vunit = u.x;
-              vinv = u.y;
-            }
             uneven = __any_sync(0xffffffffu, uneven) || x > least * TR_V_EVEN;
-            if (!uneven) vtop = fmaxf(vtop, fminf(x, vunit * (TR_V_MOST / TR_V_EVEN)));  // a few large ones, that no row may see, are looked at again
-            if (mine_v * vinv > TR_V_MOST) mine_v = __uint_as_float(0x7fc00000u);
+            if (!uneven) vtop = fmaxf(vtop, x);  // a few large ones, that no row may see, are looked at again
           }
           const bool bad = key < Ltot && !(fabsf(mine_v) + fabsf(mine_k) < INFINITY);
           // Where some row does not see some key, that key's scales may be anything (a slot that was never written has zeros), but neither may
           // make a NaN of a score of -inf or of a weight of 0: the key's is positive and finite (the rows that see a key whose scale is zero
           // get its scores, zeros, from the smallest one), a value's finite, and the rows that do see a key with others are marked.
           if (part == 0) sc[i] = plain || (key < Ltot && !bad && mine_k > 0.f) ? mine_k : 1.17549435e-38f;
-          else sc[TW_KEYS + i] = plain || !bad ? mine_v * vinv : 0.f;
+          else sc[TW_KEYS + i] = plain || !bad ? mine_v : 0.f;
           if (!plain) {
             const unsigned m = __ballot_sync(0xffffffffu, bad);
             if (lane == 0) reinterpret_cast<volatile uint32_t*>(&s_bad[st][part])[warp & 1] = m;
           }
           hand_over(st);  // the softmax warps have left step t - 2: the V part of step t - 1 has waited for its product
-          if (pt == 0) {
-            s_vtop[t & 1] = uneven ? -INFINITY : value_log2(x * vinv);
-            s_vunit = vunit;
-          }
+          if (pt == 0) s_vtop[t & 1] = uneven ? -INFINITY : value_log2(x);
         }
         if (pt == 0) s_groups[st] = ngl;
         fence_proxy_async_smem();
@@ -682,14 +673,14 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
         float fix = 1.f;
         bool moved = false;
         if (mx > m_used + (m_used == -INFINITY ? 0.f : TR_RESCALE)) {
-          fix = m_used == -INFINITY ? 0.f : tr_ex2(m_used - mx);
+          fix = m_used == -INFINITY ? 0.f : tr_ex2(F16 ? 0.5f * (m_used - mx) : m_used - mx);  // 8-bit: its root, since it may pass the range of a float
           m_used = mx;
           moved = true;
         }
         const float bias = F16 ? TR_P_SHIFT - (m_used == -INFINITY ? 0.f : m_used) : (m_used == -INFINITY ? 0.f : -m_used);
         if (__any_sync(0xffffffffu, moved)) {
-          l2.x *= fix;
-          l2.y *= fix;
+          l2.x = F16 ? l2.x * fix * fix : l2.x * fix;
+          l2.y = F16 ? l2.y * fix * fix : l2.y * fix;
           if (t > 0) {
             if (!warp_wait(odone((t - 1) & 1), ((t - 1) >> 1) & 1)) { fail_site = 77; ok = false; break; }
             tc_fence_after();
@@ -699,7 +690,7 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
               tc_ld8(tO + lanes + c, o);
               tc_wait_ld_pin(o);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) o[k] *= fix;
+              for (int k = 0; k < 8; ++k) o[k] = F16 ? o[k] * fix * fix : o[k] * fix;
               tc_st8(tO + lanes + c, o);
             }
           }
@@ -733,12 +724,13 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
       if (ok && mine > 0 && !warp_wait(odone((mine - 1) & 1), ((mine - 1) >> 1) & 1)) { fail_site = 78; ok = false; }
       tc_fence_after();
       if (ok) {
-        const float l = l2.x + l2.y, vunit = F16 ? (mine > 0 ? s_vunit : 0.f) : 1.f;
+        const float l = l2.x + l2.y;
         bool odd = false;
         const int row = row0 + rr;
         const int64_t o = ((int64_t)b * P.Hq + hkv * G + row % G) * T + row / G, at = (grp * P.nsplit + split) * (int64_t)(T * G) + row;
         const bool direct = P.nsplit == 1;
-        const float f = direct ? (l > 0.f || l != l ? vunit / l : 0.f) : vunit;
+        const float f = direct || F16 ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;  // 8-bit: see the parts of atf_tree_tiles
+        const float ref = F16 ? m_used + log2f(l) - TR_P_SHIFT : m_used;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           float x[32];  // dims c .. c + 31
@@ -777,8 +769,8 @@ atf_tree_wide(const __grid_constant__ CUtensorMap tmV, const __grid_constant__ T
           for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4*>(P.O + o * D + c) = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
         }
         if (rr < rows) {
-          if (!direct) *reinterpret_cast<float2*>(P.sums + at * 2) = make_float2(m_used, l);
-          else if (P.lse) P.lse[o] = odd ? __uint_as_float(0x7fc00000u) : (m_used + log2f(l) - (F16 ? TR_P_SHIFT : 0.f)) * 0.6931471805599453f;
+          if (!direct) *reinterpret_cast<float2*>(P.sums + at * 2) = F16 ? make_float2(l == 0.f ? -INFINITY : ref, l == 0.f ? 0.f : 1.f) : make_float2(m_used, l);
+          else if (P.lse) P.lse[o] = odd ? __uint_as_float(0x7fc00000u) : (F16 ? ref : m_used + log2f(l)) * 0.6931471805599453f;
         }
       }
       }

@@ -38,6 +38,7 @@ def _check(fmt, Q, K, V, W, O, LSE, nodes, parents=PARENTS, length=L):
     that largest product a key, times a code of at most 448 (or 127), where 448 times a scale is less than 2 max|v| of the row
     of values (127 times a scale: (1 + 2^-7) max|v|).  2^-25 of the largest p max|v| among the keys that the row sees, a key."""
     k, v = (ref.held(t[0, :, :length + len(parents)].double().cpu().numpy(), fmt) for t in (K, V))
+    apart = np.abs(np.log2(v[1])).max()
     k, v = k[0] * k[1][..., None], v[0] * v[1][..., None]
     G, h = Q.shape[1] // HKV, D // 2
     depth, line = ref.tree(parents)
@@ -60,6 +61,8 @@ def _check(fmt, Q, K, V, W, O, LSE, nodes, parents=PARENTS, length=L):
             p /= p.sum()
             A = (np.abs(kk) @ np.abs(qq)).max() / np.sqrt(D)
             w, u = 2.0 ** -18 * A + 2.0 ** -20, (len(ks) / 8 + 64) * 2.0 ** -24
+            if fmt != "bf16":
+                w += 2.0 ** -22 * apart
             assert abs(lse[hq, i] - rl) <= w + u + 2.0 ** -20 * abs(rl), (i, hq, lse[hq, i], rl)
             tol = (2.0 ** (-8 if fmt == "bf16" else -11) + 2 * w + 2 * u) * (p @ np.abs(vv)) + 2.0 ** -8 * np.abs(p @ vv) * 1.001
             if fmt != "bf16":
@@ -98,7 +101,7 @@ def test_slots_that_were_never_written(fmt, G, scale):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("G", ROWS)
-@pytest.mark.parametrize("byte", [0x7f, 0xff, 0x80, 0x55])
+@pytest.mark.parametrize("byte", [0x7f, 0xff, 0x80, 0x55, 0x7e, 0x01])
 def test_bytes_of_slots_that_were_never_written(fmt, G, byte):
     """0x7f and 0xff are the NaN of e4m3, which no row that is written gets, and of a bf16 bytewise."""
     K, V, Q = _inputs(G)
@@ -159,6 +162,23 @@ def test_rows_of_zeros_among_small_values(fmt, G, power, zeros):
     at = torch.arange(CAP, device="cuda")
     none = {"one": at == 150, "first": at < 140, "most": at % 9 != 4}[zeros]
     V = torch.where(none[:, None], torch.zeros_like(V), (V.double() * 2.0 ** power).to(torch.bfloat16))
+    c = atf.new_kvcache(1, HKV, CAP, D, fmt)
+    atf.atf_kvcache_write(c, K, V)
+    O, LSE = _attend(c, Q, None)
+    _check(fmt, Q, K, V, [CAP] * (D // 2), O, LSE, range(T))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G", ROWS)
+@pytest.mark.parametrize("zeros", ["first", "last"])
+@pytest.mark.parametrize("low,high", [(-45, 45), (45, -45), (-90, -20), (100, 100)])
+def test_rows_of_zeros_beside_sizes_that_change(fmt, G, zeros, low, high):
+    """Whole blocks of zeros, whose weights count in every sum, beside values whose size changes along the text."""
+    K, V, Q = _inputs(G)
+    at = torch.arange(CAP, device="cuda")
+    none = at < 140 if zeros == "first" else at >= 170
+    power = low + (high - low) * at.double() / CAP
+    V = torch.where(none[:, None], torch.zeros_like(V), (V.double() * torch.exp2(power)[:, None]).to(torch.bfloat16))
     c = atf.new_kvcache(1, HKV, CAP, D, fmt)
     atf.atf_kvcache_write(c, K, V)
     O, LSE = _attend(c, Q, None)
