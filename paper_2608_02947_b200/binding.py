@@ -758,7 +758,9 @@ def _tree_scratch(fmt, B, Hq, Hkv, T, max_len, d):
 def atf_decode_tree(Q, cache, lens, parents=None, table=None, counts=None, max_len=None, return_lse=False, O=None, LSE=None):
     """Windowed attention of T drafted tokens per sequence, Q [B,Hq,T,d] (CUDA bf16, rotated at lens + depth), over a KVCache
     whose first lens[b] slots are committed and whose next T hold the drafted keys and values.
-    lens: int32 [B] on the GPU (with max_len, the most any of them is; default: what the cache has room for), or one int.
+    lens: int32 [B] on the GPU (with max_len, the most any of them is; default: what the cache has room for), or one int.  The work
+    is split for max_len: where the cache is much larger than its text, give it (1000 tokens in 131072 slots: 14 instead of 11 us
+    for one node, 51 instead of 35 for 32).
     parents: int32 [T] or [B,T], the node each follows (-1: the committed text); None: a chain.  counts: int32 [B], nodes of
     each sequence; rows of O and LSE behind them stay as they are.  Returns O [B,Hq,T,d], or (O, LSE [B,Hq,T])."""
     if not (isinstance(Q, torch.Tensor) and Q.dtype is torch.bfloat16 and Q.is_cuda and Q.is_contiguous()):

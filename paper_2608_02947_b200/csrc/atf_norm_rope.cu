@@ -171,8 +171,8 @@ __global__ void __launch_bounds__(NR_THREADS, U * (int)sizeof(T) > 4 ? 2 : 3) at
 }
 
 // A prompt gives a thread all heads of its token, eight of them (four in fp32) in flight: bound by memory (24/8 heads of 128 x 32768, bf16,
-// 537 MB: two heads in flight 100 us, four 93, eight 87; 6.2 TB/s).  Fewer tokens have their heads dealt over blocks, two (one) at a
-// time, since what a thread looks at behind the last head costs it as much as a head (8 tokens: 4.0 us, with eight at a time 6.6), and
+// 537 MB: two heads in flight 100 us, four 93, eight 89; 6.1 TB/s).  Fewer tokens have their heads dealt over blocks, two (one) at a
+// time, since what a thread looks at behind the last head costs it as much as a head (8 tokens: 4.1 us, with eight at a time 6.6), and
 // very few over the threads of a block as well (132 tokens of 28/4 heads: 4.5 us; 5001 of 14/2 heads of 64 in fp32: 9.7, and 11.0
 // where the threads of a block share the heads although there are blocks enough).
 template <int D, typename T>
